@@ -91,7 +91,9 @@ __global__ __launch_bounds__(kThreads, 2) void ssm_bwd_kernel(SsmParams p)
         for (int i = 0; i < 4; ++i) own[0][tid][i] = own[1][tid][i] = 0.0f;
     if (!empty) {
     Place at = Place::of(p.seq, it.t1 - 1);
-    int stop = it.t0;                                // chunks down to the one that holds this token
+    // Down to the chunk that holds the run's first token of a sequence.  Of those before it there are no states: a forward run without
+    // such a token leaves them as they were, and runs of the two directions begin at different tokens.
+    const int stop = it.t0 + (from - it.t0) / CT * CT, chunk_stop = it.chunk0 + (stop - it.t0) / CT;
     if (ENDS) {
         const Place start = Place::of(p.seq, from);
         if (start.beg >= from) return;               // the run's first token begins a sequence: nothing of it reaches the runs before
@@ -110,13 +112,13 @@ __global__ __launch_bounds__(kThreads, 2) void ssm_bwd_kernel(SsmParams p)
         par[tid / kSsmChannels][ch] = from && ch < it.nd ? from[it.d0 + ch] : 0.0f;
     }
     SsmStage<IO, SP, CT, WHOLE> st;
-    int tc = it.t0 + (n_chunks - 1) * CT;
+    int tc = stop + (n_chunks - 1) * CT;
     st.template load<true, GATE>(p, it, tc);
     if (it.nd < kSsmChannels)
         for (int e = tid; e < CT * kSsmChannels; e += kThreads) (&du[0][0])[e] = float4{};
     __syncthreads();
     float h_next[SPL];
-    if (!ENDS) load_states<SPL>(h_next, p.saved + (size_t)(it.chunk0 + n_chunks - 1) * p.D * p.S, d, p.S, s0);
+    if (!ENDS) load_states<SPL>(h_next, p.saved + (size_t)(chunk_stop + n_chunks - 1) * p.D * p.S, d, p.S, s0);
     for (int n = n_chunks - 1; n >= 0; --n, tc -= CT) {
         const bool real = st.real;
         if (CT * 16 >= kThreads || stok < CT)
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(kThreads, 2) void ssm_bwd_kernel(SsmParams p)
             if (e < 2 * CT * SP) (&bc[0][0][0])[e] = st.there[k] ? (float)st.bc[k] : 0.0f;
         }
         __syncthreads();
-        st.template load<true, GATE>(p, it, max(tc - CT, it.t0));        // (always, as in the forward walk)
+        st.template load<true, GATE>(p, it, max(tc - CT, stop));        // (always, as in the forward walk)
         if constexpr (ENDS) {
             auto back = [&](int i) {
                 const float4 o = du[i][cl];
@@ -174,7 +176,7 @@ __global__ __launch_bounds__(kThreads, 2) void ssm_bwd_kernel(SsmParams p)
             float h_in[SPL], hs[CT][SPL], a[KEEP ? CT : 1][SPL];
 #pragma unroll
             for (int k = 0; k < SPL; ++k) h_in[k] = h_next[k];
-            load_states<SPL>(h_next, p.saved + (size_t)(it.chunk0 + max(n - 1, 0)) * p.D * p.S, d, p.S, s0);
+            load_states<SPL>(h_next, p.saved + (size_t)(chunk_stop + max(n - 1, 0)) * p.D * p.S, d, p.S, s0);
             auto walk = [&](auto EDGE) {
                 constexpr bool edge = decltype(EDGE)::value;
                 uint32_t firsts = 0, lasts = 0;
