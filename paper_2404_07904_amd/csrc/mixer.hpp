@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "ssm_walk.hpp"
+
 namespace hgrn2 {
 
 // Sequences on a token axis of T tokens: B of N tokens each (cu null, T = B N), or cu[b] .. cu[b + 1] - 1 for sequence b.
@@ -25,7 +27,7 @@ struct Sequences {
 // The sequence a wave is in as it walks along the token axis.  All values are the same in every lane.
 struct Place {
     int b, beg, end;
-    // the last sequence that starts at token t or before (64 lanes look at 64 offsets at a time)
+    // the last sequence that starts at token t or before, t < s.last() (64 lanes look at 64 offsets at a time): beg <= t < end
     __device__ __forceinline__ static Place of(const Sequences& s, int t)
     {
         int b = 0;
@@ -45,8 +47,8 @@ struct Place {
         }
         Place p;
         p.b = b;
-        p.beg = s.start(b);
-        p.end = max(s.start(b + 1), p.beg);
+        p.beg = place_first(s.start(b), t);
+        p.end = place_end(s.start(b + 1), t, s.last());
         return p;
     }
     __device__ __forceinline__ void forward_to(const Sequences& s, int t)

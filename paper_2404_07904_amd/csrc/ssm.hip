@@ -64,19 +64,23 @@ __global__ __launch_bounds__(kThreads) void ssm_fwd_kernel(SsmParams p)
         });
     }
     if (WALK == kSsmOut && p.zero_rest) ssm_zero_rest<WHOLE>(p, it, static_cast<IO*>(p.y));
-    int tc = it.t0;
     if (it.t1 <= max(it.t0, it.lo)) return;
-    Place at = Place::of(p.seq, max(tc, it.lo));
+    Place at = Place::of(p.seq, max(it.t0, it.lo));
+    SsmChunks chunks = ssm_chunks_forward(it.t0, it.t1, CT);
     if (WALK == kSsmEnds) {
         // nobody asks for the state behind the last token of a sequence, nor for what was before that token's sequence began
-        Place end = Place::of(p.seq, it.t1 - 1);
+        const Place end = Place::of(p.seq, it.t1 - 1);
         if (end.end <= it.t1) return;
-        if (end.beg > tc) { tc += (end.beg - tc) / CT * CT; at = end; if (tc < end.beg) at = Place::of(p.seq, max(tc, it.lo)); }
+        if (end.beg > it.t0) {
+            chunks = ssm_chunks_to_end(it.t0, it.t1, end.beg, CT);
+            at = chunks.first < end.beg ? Place::of(p.seq, max(chunks.first, it.lo)) : end;
+        }
     } else if (at.beg < it.t0) {
-        const int first_run = p.seq.cu ? at.beg / p.run_len : it.run - it.run % p.runs;
+        const int first_run = p.seq.cu ? ssm_first_run(at.beg, p.run_len) : it.run - it.run % p.runs;
         chain_before<SPL>(p, it.run, first_run, d, s0, A2, h);
     }
-    const int n_chunks = (it.t1 - tc + CT - 1) / CT;
+    int tc = chunks.first;
+    const int n_chunks = chunks.count;
     const int stok = tid >> 4, sc = four_of(tid, it.nd);
     float bias[4], skip[4];
     load_row<float, 4>(p.dt_bias ? p.dt_bias + it.d0 + sc : p.A, p.dt_bias ? it.nd - sc : 0, bias);

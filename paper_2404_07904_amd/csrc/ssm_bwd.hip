@@ -91,21 +91,19 @@ __global__ __launch_bounds__(kThreads, 2) void ssm_bwd_kernel(SsmParams p)
         for (int i = 0; i < 4; ++i) own[0][tid][i] = own[1][tid][i] = 0.0f;
     if (!empty) {
     Place at = Place::of(p.seq, it.t1 - 1);
-    // Down to the chunk that holds the run's first token of a sequence.  Of those before it there are no states: a forward run without
-    // such a token leaves them as they were, and runs of the two directions begin at different tokens.
-    const int stop = it.t0 + (from - it.t0) / CT * CT, chunk_stop = it.chunk0 + (stop - it.t0) / CT;
     if (ENDS) {
         const Place start = Place::of(p.seq, from);
         if (start.beg >= from) return;               // the run's first token begins a sequence: nothing of it reaches the runs before
         if (start.end < it.t1) {                     // only the tokens of that sequence do
-            it.t1 = start.end;
+            it.t1 = ssm_end_back(it.t1, start.end);
             at = start;
         }
     } else if (at.end > it.t1) {
-        const int last_run = p.seq.cu ? (at.end - 1) / p.run_len : it.run - it.run % p.runs + p.runs - 1;
+        const int last_run = p.seq.cu ? ssm_last_run(at.end, p.run_len) : it.run - it.run % p.runs + p.runs - 1;
         chain_behind<SPL>(p, it.run, last_run, d, s0, A2, c);
     }
-    const int n_chunks = (it.t1 - stop + CT - 1) / CT;
+    const SsmChunks chunks = ssm_chunks_back(it.t0, it.lo, it.t1, CT);
+    const int stop = chunks.first, n_chunks = chunks.count, chunk_stop = it.chunk0 + (stop - it.t0) / CT;
     if (tid < 2 * kSsmChannels) {
         const float* from = tid < kSsmChannels ? p.dt_bias : p.Dskip;
         const int ch = tid % kSsmChannels;

@@ -174,29 +174,30 @@ struct SsmStage {
     {
         return reinterpret_cast<const T*>(reinterpret_cast<const char*>(p) + bytes);
     }
-    __device__ __forceinline__ void offsets(const SsmParams& p, const SsmItem& it, int first, int last)     // tokens of the chunk that may be read
+    __device__ __forceinline__ void offsets(const SsmParams& p, const SsmItem& it, SsmTokens in)
     {
-        const int tid = (int)threadIdx.x, tok = min(max(tid >> 4, first), last), c = four_of(tid, it.nd);
+        const int tid = (int)threadIdx.x, tok = ssm_chunk_token(tid >> 4, in), c = four_of(tid, it.nd);
         constexpr uint32_t E = sizeof(IO);
         ox = (uint32_t)tok * (uint32_t)p.ldx * E + c * E;
         odt = (uint32_t)tok * (uint32_t)p.lddt * E + c * E;
         oz = (uint32_t)tok * (uint32_t)p.ldz * E + c * E;
         og = (uint32_t)tok * (uint32_t)p.ldg * E + c * E;
-        real = tid >> 4 >= first && tid >> 4 <= last;
+        real = tid >> 4 >= in.first && tid >> 4 <= in.last;
 #pragma unroll
         for (int k = 0; k < NBC; ++k) {
-            const int e = tid + k * kThreads, i = e / SP % CT, s = e % SP, j = min(max(i, first), last);
+            const int e = tid + k * kThreads, i = e / SP % CT, s = e % SP, j = ssm_chunk_token(i, in);
             obc[k] = (uint32_t)j * (uint32_t)(e / (CT * SP) & 1 ? p.ldc : p.ldb) * E + min(s, p.S - 1) * E;
-            there[k] = s < p.S && i >= first && i <= last;
+            there[k] = s < p.S && i >= in.first && i <= in.last;
         }
     }
     template <bool G, bool Z>
     __device__ __forceinline__ void load(const SsmParams& p, const SsmItem& it, int tc)
     {
-        const int from = max(it.t0, it.lo) - tc, upto = it.t1 - 1 - tc;
-        if (from > 0 || upto < CT - 1 || changed) {
-            offsets(p, it, max(from, 0), min(upto, CT - 1));
-            changed = from > 0 || upto < CT - 1;
+        const SsmTokens in = ssm_tokens_of(tc, it.t0, it.lo, it.t1, CT);
+        const bool part = in.first > 0 || in.last < CT - 1;
+        if (part || changed) {
+            offsets(p, it, in);
+            changed = part;
         }
         x = four(at(static_cast<const IO*>(p.x) + (size_t)tc * p.ldx + it.d0, ox), it);
         dt = four(at(static_cast<const IO*>(p.dt) + (size_t)tc * p.lddt + it.d0, odt), it);
