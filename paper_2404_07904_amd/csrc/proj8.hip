@@ -7,11 +7,17 @@
 // themselves, so a sum runs through the whole contraction in its fp32 accumulators; they are 2^(byte - 127) per row and block of 32, and all
 // four blocks of a block of 128 get the same byte.  (Which 32 of the 128 values of a step a lane holds does not matter then, as long as
 // both operands have the same ones.)
-// Precision: these instructions add the products eight by eight and cut off what lies 2^-13 below the largest of the eight; from there on sums are fp32.
+// Precision: these instructions (and the unscaled ones in 8 bits alike) add the products eight by eight and cut off what lies 2^-13 below the largest of the
+// eight, 1.5e-5 of a sum of random terms at any length; from there on sums are fp32.  Results in bf16, whose own rounding is up to 2^-8, are such sums, with the
+// same eights in every kernel: one token's result and the same token's among many differ by the order of fp32 additions only.  Results in fp32 are exact sums: a
+// value of e4m3 times its scale is a value of bf16, so their fragments are converted on the way from LDS to the bf16 instructions, which add
+// products in fp32 (4e-8 at K = 1024, as fp32 additions one after the other).
 //
 // Bound by the matrix units where rows are many: 16384 x 2048 x 8192 (M, N, K) 220 us, 2.5 PFLOP/s, the steady state of the steps; with K = 2048
-// the start and end of a tile, which nothing hides, bring 16384 x 8192 to 2.1 PFLOP/s (260 us).  Four waves of 128 x 128 instead of eight of 128 x 64:
-// 226 us for 220.  Hundreds of rows: bound by the time of few steps on part of the units.  Few rows: by reading B.
+// the start and end of a tile, which are not overlapped with another's, bring 16384 x 8192 to 2.1 PFLOP/s (260 us).  Four waves of 128 x 128 instead of
+// eight of 128 x 64: 226 us for 220.  Exact sums: bound by the conversions, 16 cycles for two values a lane, of which a wave of 128 x 128 needs the fewest next to
+// its products: 2048 x 8192 x 16384 385 us, 1.43 PFLOP/s (tiles of 128 x 128 546; in bf16 217).  Hundreds of rows: bound by the time of few steps on part of the
+// units.  Few rows: by reading B (in fp32 1 x 8192 x 2048 5.0 us, in bf16 4.8).
 #include <type_traits>
 
 #include "../../include/hgrn2.h"
@@ -23,6 +29,17 @@ namespace hgrn2 {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// Exact sums: 32 bytes of a row and their scale become four fragments of the bf16 instructions.  All values are taken at half their size: the largest,
+// 2^128, is then a number of bf16 too; sums come out a quarter of theirs.
+constexpr float kExactBack = 4.0f;
+__device__ __forceinline__ float exact_scale(int byte) { return __uint_as_float((uint32_t)(byte - 1) << 23); }
+__device__ __forceinline__ bf16x8 exact_part(const i32x8& f, int u, float scale)
+{
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * u], scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * u], scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * u + 1], scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * u + 1], scale, true);
+    return __builtin_shufflevector(__builtin_shufflevector(a, b, 0, 1, 2, 3), __builtin_shufflevector(c, d, 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
+}
 
 struct Proj8Params {
     const uint8_t *A, *B, *sa, *sb;
@@ -77,12 +94,14 @@ constexpr int scale_places(int ns) { return ns <= 4 ? 2 : 4; }
 // wave has that half's fragments in registers and the next step's loads, which went out NS - 1 steps ago, have landed; behind it the step's
 // place is refilled with the step NS later.  Scales come four steps at a time, a dword per row, the same way.
 template <typename OUT, int TM, int TN, int WM, int WN, int NS>
-__global__ __launch_bounds__(64 * WM * WN, 2) void proj8_tile_kernel(Proj8Params p)
+__global__ __launch_bounds__(64 * WM * WN, TM * TN / (WM * WN) > 8192 ? 1 : 2) void proj8_tile_kernel(Proj8Params p)
 {
     constexpr int NW = WM * WN, LA = TM / 8 / NW, LB = TN / 8 / NW, NI = TM / WM / 32, NJ = TN / WN / 32;
-    constexpr int STEP = (TM + TN) * 128, SCALES = NS * STEP, ROWS = TM + TN;
+    constexpr int STEP = (TM + TN) * 128, SCALES = NS * STEP, ROWS = TM + TN, LS = (ROWS / 64 + NW - 1) / NW;
+    constexpr bool EXACT = sizeof(OUT) == 4;
     static_assert((NS & (NS - 1)) == 0 && NS >= 2 && NS <= 8, "places of a power of two");
     static_assert(LA >= 1 && LB >= 1 && NI >= 1 && NJ >= 1 && ROWS % 64 == 0, "whole load instructions");
+    static_assert((NS - 1) * (LA + LB + LS) < 64, "loads that can be counted");
     typedef __attribute__((address_space(3))) void* lds_ptr;
     typedef const __attribute__((address_space(1))) void* global_ptr;
     extern __shared__ __align__(16) char smem[];
@@ -123,15 +142,19 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void proj8_tile_kernel(Proj8Params
     auto load_b = [&](int at, int ks, int j) {
         __builtin_amdgcn_global_load_lds((global_ptr)(bbase + (size_t)min(ks, nk - 1) * 128 + bo[j]), (lds_ptr)(smem + at * STEP + TM * 128 + 8 * (LB * w + j) * 128), 16, 0, 0);
     };
-    // scales of 64 rows of the tile's A and B, four steps of them
-    const int sr = 64 * (w % (ROWS / 64));
-    const char* srow;
-    {
-        const int row = sr < TM ? min(m0 + sr + lane, p.M - 1) >> p.ra : min(n0 + sr - TM + lane, p.N - 1) >> p.rb;
-        srow = reinterpret_cast<const char*>(sr < TM ? p.sa : p.sb) + (size_t)row * p.sp + first;
+    // scales of the tile's rows of A and B, 64 rows a load and four steps of them; LS such loads a wave
+    const char* srow[LS];
+    int sr[LS];
+#pragma unroll
+    for (int j = 0; j < LS; ++j) {
+        sr[j] = 64 * ((w + j * NW) % (ROWS / 64));
+        const int row = sr[j] < TM ? min(m0 + sr[j] + lane, p.M - 1) >> p.ra : min(n0 + sr[j] - TM + lane, p.N - 1) >> p.rb;
+        srow[j] = reinterpret_cast<const char*>(sr[j] < TM ? p.sa : p.sb) + (size_t)row * p.sp + first;
     }
     auto load_scales = [&](int ks) {
-        __builtin_amdgcn_global_load_lds((global_ptr)(srow + (min(ks, nk - 1) & ~3)), (lds_ptr)(smem + SCALES + ((ks >> 2) & (scale_places(NS) - 1)) * ROWS * 4 + sr * 4), 4, 0, 0);
+#pragma unroll
+        for (int j = 0; j < LS; ++j)
+            __builtin_amdgcn_global_load_lds((global_ptr)(srow[j] + (min(ks, nk - 1) & ~3)), (lds_ptr)(smem + SCALES + ((ks >> 2) & (scale_places(NS) - 1)) * ROWS * 4 + sr[j] * 4), 4, 0, 0);
     };
     f32x16 acc[NI][NJ];
 #pragma unroll
@@ -163,10 +186,23 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void proj8_tile_kernel(Proj8Params
         for (int j = 0; j < NJ; ++j) sb[j] = s[(TM + (TN / WN) * wn + 32 * j + r32) * 4];
     };
     constexpr int NL = LA + LB;
+    bf16x8 wb[EXACT ? NJ : 1][4];
     auto multiply = [&](int kk, int i) {
+        if constexpr (EXACT) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[kk][j], fa[i], acc[i][j], 0, 0, 0, sb[j], 0, sa[i]);
+            for (int u = 0; u < 4; ++u) {
+                const bf16x8 wa = exact_part(fa[i], u, exact_scale(sa[i]));
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    if (i == 0) wb[j][u] = exact_part(fb[kk][j], u, exact_scale(sb[j]));
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j][u], wa, acc[i][j], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[kk][j], fa[i], acc[i][j], 0, 0, 0, sb[j], 0, sa[i]);
+        }
     };
     auto refill = [&](int at, int ks, int j) { if (j < LB) load_b(at, ks, j); else load_a(at, ks, j - LB); };
 #pragma unroll
@@ -177,7 +213,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void proj8_tile_kernel(Proj8Params
     }
     // all but the youngest n of this wave's loads have landed, and all its LDS reads
     constexpr auto landed = [](int n) { return (n & 15) | ((n >> 4) << 14) | 0x0070; };
-    __builtin_amdgcn_s_waitcnt(landed((NS - 1) * (NL + 1)));
+    __builtin_amdgcn_s_waitcnt(landed((NS - 1) * (NL + LS)));
     __builtin_amdgcn_s_barrier();
     read_scales(0);
     read_b(0, 0);
@@ -202,7 +238,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void proj8_tile_kernel(Proj8Params
         __builtin_amdgcn_sched_barrier(0);
         multiply(1, 0);
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(landed((NS - 2) * (NL + 1)));           // this wave's loads of the next step, its fragments of this one
+        __builtin_amdgcn_s_waitcnt(landed((NS - 2) * (NL + LS)));           // this wave's loads of the next step, its fragments of this one
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         read_b(behind, 0);
@@ -256,7 +292,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void proj8_tile_kernel(Proj8Params
                 const f32x4 lo = *reinterpret_cast<const f32x4*>(stage + (r + lane / PER) * PITCH + c), hi = *reinterpret_cast<const f32x4*>(stage + (r + lane / PER) * PITCH + c + 4);
                 float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = proj8_act<decltype(ACT)::value>((e < 4 ? lo[e & 3] : hi[e & 3]) + bias[e]);
+                for (int e = 0; e < 8; ++e) v[e] = proj8_act<decltype(ACT)::value>((EXACT ? kExactBack : 1.0f) * (e < 4 ? lo[e & 3] : hi[e & 3]) + bias[e]);
                 T* to = out + (size_t)m * p.N + n;
                 if (whole || m < p.M) {
                     if (whole || n + 8 <= p.N) store_eight(to, v);
@@ -315,6 +351,7 @@ template <typename OUT, int MI>
 __global__ __launch_bounds__(512) void proj8_rows_kernel(Proj8Params p)
 {
     constexpr int W = 8;
+    constexpr bool EXACT = sizeof(OUT) == 4;
     __shared__ __align__(16) f32x4 red[W][MI][64];
     const int tid = (int)threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -340,7 +377,14 @@ __global__ __launch_bounds__(512) void proj8_rows_kernel(Proj8Params p)
         const int eb = sb[k];
 #pragma unroll
         for (int i = 0; i < MI; ++i)
-            acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, vec(a[i] + (size_t)k * 128), acc[i], 0, 0, 0, eb, 0, (int)sa[i][k]);
+            if constexpr (EXACT) {
+                const i32x8 fa = vec(a[i] + (size_t)k * 128);
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(exact_part(fb, u, exact_scale(eb)), exact_part(fa, u, exact_scale(sa[i][k])), acc[i], 0, 0, 0);
+            } else {
+                acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, vec(a[i] + (size_t)k * 128), acc[i], 0, 0, 0, eb, 0, (int)sa[i][k]);
+            }
     }
 #pragma unroll
     for (int i = 0; i < MI; ++i) red[w][i][lane] = acc[i];
@@ -355,7 +399,7 @@ __global__ __launch_bounds__(512) void proj8_rows_kernel(Proj8Params p)
             const int left = p.N - n;
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = proj8_act(p.act, s[e] + (p.bias ? p.bias[min(n + e, p.N - 1)] : 0.0f));
+            for (int e = 0; e < 4; ++e) v[e] = proj8_act(p.act, (EXACT ? kExactBack : 1.0f) * s[e] + (p.bias ? p.bias[min(n + e, p.N - 1)] : 0.0f));
             store_row<OUT, 4>(static_cast<OUT*>(p.C) + (size_t)m * p.N + n, left, v);
         }
     }
@@ -384,8 +428,10 @@ template <typename OUT> hipError_t launch_proj8(const Proj8Params& p, const Proj
         else proj8_rows_kernel<OUT, 4><<<grid, 512, 0, st>>>(p);
         return hipGetLastError();
     }
-    hipError_t e = plan.tile == 256 ? launch_tile<OUT, 256, 256, 2, 4, 2>(p, st) : plan.tile == 128 ? launch_tile<OUT, 128, 128, 2, 2, 4>(p, st)
-                                                                                               : launch_tile<OUT, 64, 64, 2, 2, 8>(p, st);
+    hipError_t e;
+    if (plan.tile == 64) e = launch_tile<OUT, 64, 64, 2, 2, 8>(p, st);
+    else if (plan.tile == 128) e = launch_tile<OUT, 128, 128, 2, 2, 4>(p, st);
+    else e = launch_tile<OUT, 256, 256, 2, sizeof(OUT) == 4 ? 2 : 4, 2>(p, st);
     if (e != hipSuccess || p.splits == 1) return e;
     proj8_sums_kernel<OUT><<<dim3((unsigned)(((size_t)p.M * p.N + 4 * kThreads - 1) / (4 * kThreads))), kThreads, 0, st>>>(p);
     return hipGetLastError();
@@ -412,8 +458,9 @@ extern "C" {
 size_t hgrn2_proj8_workspace_bytes(int32_t M, int32_t N, int32_t K)
 {
     if (proj8_check(M, N, K, HGRN2_BF16) != HGRN2_OK || M == 0 || N == 0) return 0;
-    const Proj8Plan plan = plan_proj8(M, N, hgrn2_quant8_pitch(K) / 128);
-    return plan.splits > 1 ? ((size_t)plan.splits * M * N * 4 + 255) & ~(size_t)255 : 0;
+    // (of either type of results)
+    const int steps = hgrn2_quant8_pitch(K) / 128, a = plan_proj8(M, N, steps).splits, b = plan_proj8(M, N, steps, true).splits, splits = a > b ? a : b;
+    return splits > 1 ? ((size_t)splits * M * N * 4 + 255) & ~(size_t)255 : 0;
 }
 
 int hgrn2_proj8(int32_t M, int32_t N, int32_t K, const uint8_t* a, const uint8_t* a_scale, int32_t a_rows, const uint8_t* b, const uint8_t* b_scale,
@@ -427,7 +474,7 @@ int hgrn2_proj8(int32_t M, int32_t N, int32_t K, const uint8_t* a, const uint8_t
     if (!a || !a_scale || !b || !b_scale || !c) return HGRN2_ERR_NULL;
     if ((((uintptr_t)a | (uintptr_t)b) & 15) || (((uintptr_t)a_scale | (uintptr_t)b_scale) & 3)) return HGRN2_ERR_UNSUPPORTED;
     const int pitch = hgrn2_quant8_pitch(K);
-    const Proj8Plan plan = plan_proj8(M, N, pitch / 128);
+    const Proj8Plan plan = plan_proj8(M, N, pitch / 128, out_dtype == HGRN2_F32);
     if (plan.splits > 1 && (!ws || ws_bytes < hgrn2_proj8_workspace_bytes(M, N, K) || ((uintptr_t)ws & 255))) return HGRN2_ERR_WORKSPACE;
     Proj8Params p{a, b, a_scale, b_scale, M, N, pitch, hgrn2_quant8_scale_pitch(K), a_rows == 128 ? 7 : 0, b_rows == 128 ? 7 : 0, bias, act, c,
                   static_cast<float*>(ws), plan.splits};

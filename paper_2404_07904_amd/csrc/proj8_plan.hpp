@@ -9,16 +9,19 @@ struct Proj8Plan { int tile, splits; };      // tile 0: the kernel for few rows
 // What a product takes with tiles of 256, 128 or 64, us, fitted to 65 to 16384 rows: a workgroup has a compute unit to itself (all three fill the
 // LDS with steps on their way), a start and an end that nothing hides, and steps that are slower the more units work at once.
 // 256 / 128 / 64: 2048^3 26.3 / 15.2 / 28.3, 4096^3 61.5 / 95.4 / 168, 128 x 8192 x 8192 36.5 / 25.2 / 21.7, 1024 x 1024 x 16384 43.4 / 32.8 / 35.3.
-inline double proj8_time(int tile, long long groups, double steps)
+// Exact sums hold the vector unit and the bf16 instructions longer: 2048^3 48.5 / 24.1 / 40.9, 4096^3 105 / 152 / 268, 128 x 8192 x 8192 157 / 68.3 / 34.5,
+// 1024 x 1024 x 16384 308 / 127 / 61.2 and in four shares 93.6 / 48.5 / 77.3.
+inline double proj8_time(int tile, long long groups, double steps, bool exact)
 {
     const double fixed = tile == 256 ? 7.0 : tile == 128 ? 4.0 : 2.2;
-    const double least = tile == 256 ? 1.0 : tile == 128 ? 0.32 : 0.23, more = tile == 256 ? 0.68 : tile == 128 ? 0.28 : 0.04;
+    const double least = exact ? (tile == 256 ? 2.3 : tile == 128 ? 0.93 : 0.41) : tile == 256 ? 1.0 : tile == 128 ? 0.32 : 0.23;
+    const double more = exact ? (tile == 256 ? 0.6 : tile == 128 ? 0.1 : 0.04) : tile == 256 ? 0.68 : tile == 128 ? 0.28 : 0.04;
     const long long rest = groups % 256;
     return 2.0 + (double)(groups / 256) * (fixed + (least + more) * steps) + (rest ? fixed + (least + more * rest / 256) * steps : 0.0);
 }
 
-// steps: blocks of 128 of the contraction
-inline Proj8Plan plan_proj8(int M, int N, int steps)
+// steps: blocks of 128 of the contraction; exact: for exact sums.
+inline Proj8Plan plan_proj8(int M, int N, int steps, bool exact = false)
 {
     if (M <= 16) return Proj8Plan{0, 1};
     Proj8Plan best{64, 1};
@@ -36,7 +39,7 @@ inline Proj8Plan plan_proj8(int M, int N, int steps)
             // (the shares are written and read once more, and added up by a launch of their own)
             const double mb = 4e-6 * M * (double)N * s;
             if (s > 1 && mb > 64.0) break;
-            const double t = proj8_time(tile, tiles * s, (double)steps / s) + (s > 1 ? 3.0 + 0.4 * mb : 0.0);
+            const double t = proj8_time(tile, tiles * s, (double)steps / s, exact) + (s > 1 ? 3.0 + 0.4 * mb : 0.0);
             if (t < least) { least = t; best = Proj8Plan{tile, s}; }
         }
     }
