@@ -467,6 +467,8 @@ int hgru2_proj_bwd(int32_t M, int32_t d, const void* x, const void* w3, const vo
  *   - Results are bit-reproducible: sums over workgroups are added in a fixed order.
  *   - Outputs overlap neither inputs nor each other, except where said.
  *   - Row pitches of the scan's tensors: at most 2^24 elements (else HGRN2_ERR_UNSUPPORTED).
+ *   - A call of which a launch would take 2^32 threads is HGRN2_ERR_UNSUPPORTED and does nothing: 2^24 workgroups of 64 channels of a run of the scan, 2^30
+ *     channels of single tokens, 2^32 elements of grad_B and grad_C; 2^30 tokens of 512 channels (fp32: 256) of the convolution; 2^35 elements to quantise.
  * Status codes, streams and ownership as everywhere in this header.
  */
 

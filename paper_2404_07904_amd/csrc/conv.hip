@@ -512,6 +512,12 @@ ConvParams conv_params(const hgrn2_conv_shape* s, const int32_t* cu, const void*
 
 int conv_tail_blocks(const hgrn2_conv_shape* s, int v) { return (int)(((long long)s->B * ((s->D + v - 1) / v) + kThreads - 1) / kThreads); }
 
+// Workgroups of a pass over the tokens, tiles of tt of them to a wave and a workgroup's 64 lanes v channels each, and of the states'.
+long long conv_groups(const hgrn2_conv_shape* s, long long tokens, int tt, int v, bool states)
+{
+    const long long tiles = (tokens + tt - 1) / tt, blocks = (s->D + 64ll * v - 1) / (64ll * v);
+    return (states ? conv_tail_blocks(s, v) : 0) + (tiles + kWaves - 1) / kWaves * blocks;
+}
 // Tokens of a wave in the reverse mode: as many tiles as leave 2048 waves, two for each vector unit, one at least, 32 at most.  Each wave fetches
 // K - 1 rows more than its own and leaves a row of sums for each tap.  With 4096 / 2048 / 1024 waves, bf16, K 4: 16384 tokens of width 4096
 // 97.6 / 91.7 / 108.4 us, 8192 of 2048 36.0 / 30.6 / 33.9, 2048 of 2048 15.8 / 15.7 / 16.3.
@@ -526,6 +532,12 @@ int conv_shares(const hgrn2_conv_shape* s, bool packed)
 {
     const long long per = (long long)kWaves * conv_span(s, packed);
     return (int)((conv_tokens(s, packed) + per - 1) / per);
+}
+
+bool conv_bwd_launchable(const hgrn2_conv_shape* s, bool packed)
+{
+    return launchable(conv_groups(s, conv_tokens(s, packed), conv_span(s, packed), kConvBackV, true), kThreads) &&
+           launchable(((s->K + 1ll) * s->D + 63) / 64, kThreads);
 }
 
 template <typename IO, int K> hipError_t launch_conv_fwd(ConvParams p, bool wide, hipStream_t st)
@@ -586,13 +598,14 @@ int hgrn2_conv_fwd(const hgrn2_conv_shape* s, const int32_t* cu, const void* x, 
     // Tiles of 16 tokens fetch 19 rows for them, tiles of 4 seven; the latter while the former are fewer than two waves for each vector unit (bf16,
     // tiles of 16 / 4: 2048 tokens of width 2048 12.0 / 8.3 us, 4096 of 2048 15.1 / 13.0, 4096 of 4096 17.2 / 21.8, 16384 of 2048 37.4 / 39.4).
     const bool wide = (long long)p.seq.T * p.blocks >= 32 * 1024;
+    if (!launchable(conv_groups(s, p.seq.T, wide && s->D >= conv_width(s) ? 16 : 4, conv_width(s), final_state != nullptr), kThreads)) return HGRN2_ERR_UNSUPPORTED;
     const hipError_t e = CONV_KERNELS(launch_conv_fwd, p, wide, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? HGRN2_OK : HGRN2_ERR_HIP;
 }
 
 size_t hgrn2_conv_bwd_workspace_bytes(const hgrn2_conv_shape* s, int32_t packed)
 {
-    if (conv_check(s, packed != 0) != HGRN2_OK) return 0;
+    if (conv_check(s, packed != 0) != HGRN2_OK || !conv_bwd_launchable(s, packed != 0)) return 0;
     return ((size_t)conv_shares(s, packed != 0) * (s->K + 1) * s->D * 4 + 255) & ~(size_t)255;
 }
 
@@ -603,6 +616,7 @@ int hgrn2_conv_bwd(const hgrn2_conv_shape* s, const int32_t* cu, const void* x, 
     const int rc = conv_check(s, packed);
     if (rc != HGRN2_OK) return rc;
     if (grad_state && grad_state == grad_final) return HGRN2_ERR_UNSUPPORTED;
+    if (!conv_bwd_launchable(s, packed)) return HGRN2_ERR_UNSUPPORTED;
     const bool work = (s->B > 0 || s->zero_rest) && conv_tokens(s, packed) > 0;
     if (!w || !grad_w || (work && (!x || !grad_y || !grad_x))) return HGRN2_ERR_NULL;
     const size_t need = hgrn2_conv_bwd_workspace_bytes(s, packed ? 1 : 0);

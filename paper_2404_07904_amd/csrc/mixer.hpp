@@ -8,6 +8,9 @@
 
 namespace hgrn2 {
 
+// A launch has fewer than 2^32 threads along an axis.
+inline bool launchable(long long groups, int threads) { return groups < (1ll << 32) / threads; }
+
 // Sequences on a token axis of T tokens: B of N tokens each (cu null, T = B N), or cu[b] .. cu[b + 1] - 1 for sequence b.
 // Offsets of a packed batch are clamped to the token axis; a wrong array can only give wrong results: every access of a kernel is
 // to a token in [0, T) that it was given, and to a sequence in [0, B).

@@ -475,6 +475,8 @@ int hgrn2_proj8(int32_t M, int32_t N, int32_t K, const uint8_t* a, const uint8_t
     if ((((uintptr_t)a | (uintptr_t)b) & 15) || (((uintptr_t)a_scale | (uintptr_t)b_scale) & 3)) return HGRN2_ERR_UNSUPPORTED;
     const int pitch = hgrn2_quant8_pitch(K);
     const Proj8Plan plan = plan_proj8(M, N, pitch / 128, out_dtype == HGRN2_F32);
+    const long long tile = plan.tile, groups = tile ? ((M + tile - 1) / tile) * ((N + tile - 1) / tile) : ((long long)N + 15) / 16;
+    if (!launchable(groups, tile == 0 || (tile == 256 && out_dtype == HGRN2_BF16) ? 512 : 256)) return HGRN2_ERR_UNSUPPORTED;
     if (plan.splits > 1 && (!ws || ws_bytes < hgrn2_proj8_workspace_bytes(M, N, K) || ((uintptr_t)ws & 255))) return HGRN2_ERR_WORKSPACE;
     Proj8Params p{a, b, a_scale, b_scale, M, N, pitch, hgrn2_quant8_scale_pitch(K), a_rows == 128 ? 7 : 0, b_rows == 128 ? 7 : 0, bias, act, c,
                   static_cast<float*>(ws), plan.splits};

@@ -282,7 +282,7 @@ int hgrn2_quant8(int32_t M, int32_t K, int32_t io_dtype, const void* x, int64_t 
 {
     if (M < 0 || K <= 0 || K > 0x7fffff00 || M > 0x7fffff00 || (io_dtype != HGRN2_F32 && io_dtype != HGRN2_BF16) || (ld_x && ld_x < K)) return HGRN2_ERR_SHAPE;
     if (block_rows != 1 && block_rows != 128) return HGRN2_ERR_UNSUPPORTED;
-    if (quant_tiles(M, K, quant_whole(block_rows == 128, q_t != nullptr)) > 0x7fffffff) return HGRN2_ERR_UNSUPPORTED;
+    if (!launchable(quant_tiles(M, K, quant_whole(block_rows == 128, q_t != nullptr)), kThreads)) return HGRN2_ERR_UNSUPPORTED;
     if (M == 0) return HGRN2_OK;
     if (!x || !q || !scale || (q_t != nullptr) != (scale_t != nullptr)) return HGRN2_ERR_NULL;
     if (((uintptr_t)q | (uintptr_t)q_t) & 15) return HGRN2_ERR_UNSUPPORTED;

@@ -291,6 +291,9 @@ constexpr size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct SsmCheck { int rc; bool packed; SsmPlan plan; };
 
+// Workgroups that add up the shares of grad_B and grad_C (n_bc elements) and of the parameters' gradients.
+long long ssm_sums_groups(long long n_bc, const hgrn2_ssm_shape* s) { return (n_bc + (long long)s->D * s->S + 2ll * s->D + kThreads - 1) / kThreads; }
+
 SsmCheck ssm_check(const hgrn2_ssm_shape* s, bool packed, bool whole, bool reverse = false)
 {
     SsmCheck c{};
@@ -312,6 +315,10 @@ SsmCheck ssm_check(const hgrn2_ssm_shape* s, bool packed, bool whole, bool rever
     }
     c.plan = ssm_plan(s->B, s->N, s->D, s->S, s->G, packed, whole, reverse, s->io_dtype == HGRN2_F32);
     if ((long long)c.plan.total * c.plan.blocks > most) { c.rc = HGRN2_ERR_SHAPE; return c; }
+    if (!launchable((long long)c.plan.total * c.plan.blocks, kThreads) || (reverse && !launchable(ssm_sums_groups(tokens * s->G * 2 * s->S, s), kThreads))) {
+        c.rc = HGRN2_ERR_UNSUPPORTED;
+        return c;
+    }
     c.rc = HGRN2_OK;
     return c;
 }
@@ -475,8 +482,7 @@ int hgrn2_ssm_bwd(const hgrn2_ssm_shape* s, const int32_t* cu, const void* x, co
     r.part_bc = p.part_bc; r.part_a = p.part_a; r.part_d = p.part_d;
     r.gB = grad_B; r.gC = grad_C; r.gA = grad_A; r.gD = grad_D; r.gbias = grad_dt_bias;
     r.n_bc = any ? (long long)p.seq.T * s->G * 2 * s->S : 0; r.n_a = (long long)s->D * s->S;
-    const long long n = r.n_bc + r.n_a + 2 * s->D;
-    const dim3 grid((unsigned)((n + kThreads - 1) / kThreads));
+    const dim3 grid((unsigned)ssm_sums_groups(r.n_bc, s));
     if (s->io_dtype == HGRN2_BF16) ssm_sums_kernel<__bf16><<<grid, kThreads, 0, st>>>(r);
     else ssm_sums_kernel<float><<<grid, kThreads, 0, st>>>(r);
     return hipGetLastError() == hipSuccess ? HGRN2_OK : HGRN2_ERR_HIP;
@@ -489,13 +495,14 @@ int hgrn2_ssm_step(const hgrn2_ssm_shape* s, const void* x, const void* dt, cons
     if (c.rc != HGRN2_OK) return c.rc;
     if (s->N != 1) return HGRN2_ERR_SHAPE;
     if (s->B == 0) return HGRN2_OK;
+    const long long groups = ((long long)s->B * s->D + 16 * kWaves - 1) / (16 * kWaves);
+    if (!launchable(groups, kThreads)) return HGRN2_ERR_UNSUPPORTED;
     if (!x || !dt || !A || !Bm || !Cm || !state || !y) return HGRN2_ERR_NULL;
     SsmParams p{};
     ssm_fill(p, s, c, nullptr);
     p.x = x; p.dt = dt; p.z = z; p.Bm = Bm; p.Cm = Cm; p.A = A; p.Dskip = D; p.dt_bias = dt_bias; p.y = y;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const long long waves = ((long long)s->B * s->D + 15) / 16;
-    const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves));
+    const dim3 grid((unsigned)groups);
     const int k = ssm_lane_states(s->S);
     if (s->io_dtype == HGRN2_BF16) {
         if (k == 2) ssm_step_kernel<__bf16, 2><<<grid, kThreads, 0, st>>>(p, state);
