@@ -50,7 +50,7 @@ inline SsmPlan ssm_plan(int B, int N, int D, int S, int G, bool packed, bool who
         if (want < 1) want = 1;
         p.len = (int)((((long long)N + want - 1) / want + 15) / 16 * 16);
         if (p.len < 16) p.len = 16;
-        p.runs = N > 0 ? (N + p.len - 1) / p.len : 1;
+        p.runs = N > 0 ? (int)(((long long)N + p.len - 1) / p.len) : 1;
     };
     cut();
     // A last round that is less than three quarters full costs more than longer runs: 3001 packed tokens of width 1030 in fp32, 846 workgroups / 504,

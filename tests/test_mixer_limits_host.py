@@ -1,9 +1,11 @@
 """Sizes past what a launch can hold (2^32 threads) are refused before the first launch of a call, without a GPU: none of these calls touches its
-pointers."""
+pointers.  And plans at the largest sizes, in which no sum of 32 bits overflows."""
 import ctypes
+import os
+import subprocess
 
 from paper_2404_07904_amd import binding
-from test_mixer_host import BIG, E_NULL, E_UNSUP, FAKE, FAKE_WS, conv, conv_bwd, conv_fwd, ssm, ssm_bwd, ssm_fwd
+from test_mixer_host import BIG, E_NULL, E_UNSUP, FAKE, FAKE_WS, ROOT, conv, conv_bwd, conv_fwd, ssm, ssm_bwd, ssm_fwd
 
 
 def test_convolution():
@@ -50,3 +52,30 @@ def test_quantisation_and_product():
 
     assert proj(1, 1 << 27) == E_UNSUP and proj(1, (1 << 27) - 16, a=None) == E_NULL
     assert proj(1 << 25, 1 << 13, K=2048, a=None) == E_NULL and proj(1 << 27, 1 << 13, K=2048) == proj(1 << 28, 1 << 15) == E_UNSUP
+
+
+PLAN = r"""
+#include <cstdio>
+#include <initializer_list>
+#include "ssm_plan.hpp"
+using namespace hgrn2;
+int main()
+{
+    for (int N : {1 << 30, (1 << 30) + 16, 0x7fffffff - 64})
+        for (int S : {8, 16, 32})
+            for (int D : {1, 4096})
+                for (int way = 0; way < 4; ++way) {
+                    const SsmPlan p = ssm_plan(1, N, D, S, 1, way == 1, way == 0, way == 2);
+                    if (p.runs < 1 || (long long)p.runs * p.len < N || (long long)(p.runs - 1) * p.len >= N || (way == 0 && p.runs != 1)) return 1;
+                    if (p.chunks != (int)(((long long)N + ssm_chunk(S) - 1) / ssm_chunk(S)) || p.total != p.runs) return 1;
+                }
+    std::puts("ok");
+}
+"""
+
+
+def test_plans_of_the_longest_sequences(tmp_path):
+    (tmp_path / "plan.cpp").write_text(PLAN)
+    subprocess.check_call(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-fsanitize=signed-integer-overflow", "-fno-sanitize-recover", "-static-libubsan",
+                           "-I", os.path.join(ROOT, "paper_2404_07904_amd", "csrc"), str(tmp_path / "plan.cpp"), "-o", str(tmp_path / "plan")])
+    assert subprocess.check_output([str(tmp_path / "plan")], text=True).strip() == "ok"
