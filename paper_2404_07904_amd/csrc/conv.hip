@@ -286,8 +286,8 @@ __global__ __launch_bounds__(kThreads, 2) void conv_bwd_kernel(ConvParams p)
         // (the last of them H tokens ahead of it), `ring` the gradients of pre of t0 + r .. t0 + r + H.
         bool carried = false;
         float in[K][V], ring[K][V];
-        // token t0 + r + H: the gradient of its pre, and its share of the parameters' sums
-        auto token = [&](int r, const float (&g)[V], float counts) {
+        // token t0 + r + H: the gradient of its pre, and its share of the parameters' sums if it counts
+        auto token = [&](int r, const float (&g)[V], bool counts) {
             float pre[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -296,13 +296,13 @@ __global__ __launch_bounds__(kThreads, 2) void conv_bwd_kernel(ConvParams p)
                 for (int k = 0; k < K; ++k) pre[i] = fmaf(taps.w[k][i], in[(r + k) % K][i], pre[i]);
             }
             through(g, pre, ring[(r + H) % K]);
+            if (counts)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float gt = counts * ring[(r + H) % K][i];
-                gb[i] += gt;
+                for (int i = 0; i < V; ++i) {
+                    gb[i] += ring[(r + H) % K][i];
 #pragma unroll
-                for (int k = 0; k < K; ++k) gw[k][i] = fmaf(gt, in[(r + k) % K][i], gw[k][i]);
-            }
+                    for (int k = 0; k < K; ++k) gw[k][i] = fmaf(ring[(r + H) % K][i], in[(r + k) % K][i], gw[k][i]);
+                }
         };
         auto edge = [&](int tb, int te) {
             constexpr int E = 4;
@@ -380,18 +380,18 @@ __global__ __launch_bounds__(kThreads, 2) void conv_bwd_kernel(ConvParams p)
                         float g[V];
                         load_row<IO, V>(x + (size_t)(t0 + r + H) * p.ldx, n, in[(r + H) % K]);
                         load_row<IO, V>(gy + (size_t)(t0 + r + H) * p.ldg, n, g);
-                        token(r + K, g, 1.0f);
+                        token(r + K, g, true);
                     }
                     carried = true;
                 }
                 // (tokens behind the last tile of a stretch are counted where their own turn comes)
-                const float last = inside(t0 + TT) ? 1.0f : 0.0f;
+                const bool last = inside(t0 + TT);
 #pragma unroll
                 for (int r = 0; r < TT; ++r) {
                     float g[V], o[V];
                     unpack(xr[r], in[(r + H) % K]);
                     unpack(gr[r], g);
-                    token(r, g, r < TT - H ? 1.0f : last);
+                    token(r, g, r < TT - H || last);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         o[i] = 0.0f;
