@@ -177,13 +177,14 @@ __global__ __launch_bounds__(kThreads, 2) void ssm_bwd_kernel(SsmParams p)
             load_states<SPL>(h_next, p.saved + (size_t)(chunk_stop + max(n - 1, 0)) * p.D * p.S, d, p.S, s0);
             auto walk = [&](auto EDGE) {
                 constexpr bool edge = decltype(EDGE)::value;
-                uint32_t firsts = 0, lasts = 0;
+                uint32_t firsts = 0, lasts = 0, real_tokens = 0;
                 if (edge) {
                     Place pl = at;
                     for (int i = CT - 1; i >= 0; --i) {
                         const int t = tc + i;
                         if (t < it.lo || t >= it.t1) continue;
                         pl.back_to(p.seq, t);
+                        real_tokens |= 1u << i;
                         firsts |= (t == pl.beg ? 1u : 0u) << i;
                         lasts |= (t + 1 == pl.end ? 1u : 0u) << i;
                     }
@@ -258,7 +259,8 @@ __global__ __launch_bounds__(kThreads, 2) void ssm_bwd_kernel(SsmParams p)
                         vc[k] = o.t.z * hs[i][k];
                         vb[k] = o.t.y * dh;
                         qs = fmaf(o.b[k], dh, qs);
-                        const float wk = c[k] * before[k];
+                        // (a token of no sequence has a step of zero, but may stand next to a state that is infinite)
+                        const float wk = !edge || (real_tokens >> i & 1) ? c[k] * before[k] : 0.0f;
                         rs = fmaf(A2[k], wk, rs);
                         gA[k] = fmaf(o.t.x, wk, gA[k]);
                     }
