@@ -24,9 +24,9 @@
 // finds every run's last state and the sum of its step sizes, all runs at once; the decay of a whole run is then one exponential per state,
 // and a run's workgroup chains the runs before it (in reverse: behind it) into the state that it starts from.
 // States and all sums are fp32.
-// 8 x 2048 tokens of width 4096 with 16 states in bf16: 390 us forward, 1.06 ms in reverse, sums of the groups' channels 32 us; a copy of what
-// they read and write takes 113 and 197 us.  The vector unit is busy for 85 and 83% of that: 31 instructions forward and 93 in reverse for each token and
-// four states, 8 x 2048 tokens of width 2048 with 8 states in half and 0.45 of the time.
+// 8 x 2048 tokens of width 4096 with 16 states in bf16: 351 us forward, 981 in reverse, sums of the groups' channels 32 us; a copy of what
+// they read and write takes 113 and 197 us.  The vector unit is busy for 86 and 81% of the waves' time: 31 instructions forward and 94 in reverse for
+// each token and four states.  8 x 2048 tokens of width 2048 with 8 states 195 and 483 us (with the walk from zero), 8 x 1024 of width 2048 with 32 states 251 and 611.
 #include "../../include/hgrn2.h"
 #include "ssm_common.hpp"
 
