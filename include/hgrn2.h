@@ -575,7 +575,8 @@ int hgrn2_quant8(int32_t M, int32_t K, int32_t io_dtype, const void* x, int64_t 
 /*
  * Matrix product of two such operands:
  *     c[m][n] = act(bias[n] + sum_k a[m][k] b[n][k])          a, b the values their bytes and scales stand for
- *   a [M][hgrn2_quant8_pitch(K)], b [N][the same]: 16-byte aligned; a_scale, b_scale: 4-byte aligned, one for a_rows, b_rows = 1 or 128 rows, bytes 1 to 254.
+ *   a [M][hgrn2_quant8_pitch(K)], b [N][the same]: 16-byte aligned; a_scale, b_scale: 4-byte aligned, one for a_rows, b_rows = 1 or 128 rows, bytes
+ *   e + 127 for 2^e (255: not a number; for fp32 results 0 counts as 1, 2^-126).
  *   The bytes behind K are part of the contraction: zeros in one operand at least, as hgrn2_quant8 leaves them.
  *   K up to 2^23 (else HGRN2_ERR_UNSUPPORTED).
  *   bias in fp32 [N] or NULL;   c out [M][N], bf16 or fp32 (out_dtype)

@@ -570,7 +570,7 @@ def hgrn2_quant8(x, *, block_rows=1, transposed=False):
 
 def hgrn2_proj8(a, a_scale, b, b_scale, bias=None, *, act=None, out_dtype=torch.bfloat16, c=None, workspace=None):
     """c [M,N] = act(a b^T + bias) of operands as hgrn2_quant8 returns them, a [M,K] and b [N,K]; act None, "silu" or
-    "sigmoid"; c bf16 or fp32."""
+    "sigmoid"; c bf16, or fp32: exact products added in fp32, at up to twice the time."""
     if act not in _ACTS:
         raise ValueError("act: None, 'none', 'silu' or 'sigmoid', not %r" % (act,))
     if out_dtype not in (torch.bfloat16, torch.float32):

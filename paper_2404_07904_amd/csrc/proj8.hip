@@ -33,7 +33,12 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 // Exact sums: 32 bytes of a row and their scale become four fragments of the bf16 instructions.  All values are taken at half their size: the largest,
 // 2^128, is then a number of bf16 too; sums come out a quarter of theirs.
 constexpr float kExactBack = 4.0f;
-__device__ __forceinline__ float exact_scale(int byte) { return __uint_as_float((uint32_t)(byte - 1) << 23); }
+// (Half of 2^(byte - 127): the conversion goes by the exponent's bits, 0 for 2^-127 and 255 for what is no number.  There is no half of byte 0, which counts as 1.)
+__device__ __forceinline__ float exact_scale(int byte)
+{
+    const int least = max(byte, 1);
+    return __uint_as_float((uint32_t)(least - (least < 255 ? 1 : 0)) << 23);
+}
 __device__ __forceinline__ bf16x8 exact_part(const i32x8& f, int u, float scale)
 {
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * u], scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * u], scale, true);

@@ -96,3 +96,26 @@ def test_bias_and_activation(M, N, K, act):
     got = lib.hgrn2_proj8(*qa, *qb, bias, act=act, out_dtype=F32).to(F64)
     # an addition and an activation in fp32: slopes of 1.1 at most, 2^-20 of the result for an exponential and a quotient
     assert ((got - ref).abs() <= 1.1 * 2.0 ** -23 * (pre.abs() + bias.abs()) + 2.0 ** -20 * ref.abs()).all()
+
+
+@pytest.mark.parametrize("M", [3, 30, 80])
+@pytest.mark.parametrize("out", [torch.bfloat16, F32])
+def test_every_byte_of_a_scale(M, out):
+    """Scales as others may write them: a block of zeros with the byte 0, the smallest and largest powers of two, and the byte that stands for no number."""
+    K = 4 * 128
+    a, b = torch.zeros(M, K, device="cuda"), torch.ones(20, K, device="cuda")
+    a[:, 256] = 1.0
+    byte = torch.full((M, 4), 127, dtype=torch.uint8, device="cuda")
+    byte[:, 0] = 0                                        # (zeros in a)
+    for e in (1, 2, 19, 127, 250, 254):
+        byte[:, 2] = e
+        other = torch.full((20, 4), 254 - e if e < 254 else 1, dtype=torch.uint8, device="cuda")
+        qa, sa, _ = operand(a, byte, 1)
+        qb, sb, _ = operand(b, other, 1)
+        want = 2.0 ** (e - 127) * 2.0 ** (float(other[0, 0]) - 127)
+        assert (lib.hgrn2_proj8(qa, sa, qb, sb, out_dtype=out).double() == want).all(), e
+    byte[:, 2], byte[1, 2] = 127, 255
+    qa, sa, _ = operand(a, byte, 1)
+    qb, sb, _ = operand(b, torch.full((20, 4), 127, dtype=torch.uint8, device="cuda"), 1)
+    c = lib.hgrn2_proj8(qa, sa, qb, sb, out_dtype=out)
+    assert torch.isnan(c[1]).all() and (c[0] == 1.0).all() and (c[2:] == 1.0).all()
