@@ -17,7 +17,7 @@
 // the start and end of a tile, which are not overlapped with another's, bring 16384 x 8192 to 2.1 PFLOP/s (260 us).  Four waves of 128 x 128 instead of
 // eight of 128 x 64: 226 us for 220.  Exact sums: bound by the conversions, 16 cycles for two values a lane, of which a wave of 128 x 128 needs the fewest next to
 // its products: 2048 x 8192 x 16384 385 us, 1.43 PFLOP/s (tiles of 128 x 128 546; in bf16 217).  Hundreds of rows: bound by the time of few steps on part of the
-// units.  Few rows: by reading B (in fp32 1 x 8192 x 2048 5.0 us, in bf16 4.8).
+// units.  Few rows: by reading B (1 x 8192 x 2048 4.7 to 5.0 us for either type).
 #include <type_traits>
 
 #include "../../include/hgrn2.h"
